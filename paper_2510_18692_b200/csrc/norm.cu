@@ -423,7 +423,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1) norm_stream_kernel(const __
         const float s1 = d1.x + d1.y, mean_d = s1 * inv_n;
         m[r] = k + mean_d;
         q[r] = fmaf(-s1, mean_d, t.x + t.y);
-      } else {                                    // fp32: the thread's mean first, then the squares around it
+      } else {                                    // fp32: the thread's mean first, then sums around it that correct it,
+                                                  // or a constant row of 1,000.1 would lie 6e-5 off its mean (0.02 in Y)
         float2 f[VPT][P];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -434,6 +435,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) norm_stream_kernel(const __
           }
         }
         m[r] = (t.x + t.y) * inv_n;
+        float2 d1 = both(0.f);
         t = both(0.f);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -441,11 +443,14 @@ __global__ void __launch_bounds__(kStreamThreads, 1) norm_stream_kernel(const __
 #pragma unroll
             for (int e = 0; e < P; ++e) {
               const float2 d = __fadd2_rn(f[i][e], both(-m[r]));
+              d1 = __fadd2_rn(d1, d);
               t = __ffma2_rn(d, d, t);
             }
           }
         }
-        q[r] = t.x + t.y;
+        const float s1 = d1.x + d1.y, fix = s1 * inv_n;
+        m[r] += fix;
+        q[r] = fmaf(-s1, fix, t.x + t.y);
       }
     }
     fetch(row + STAGES * stride, stage);   // the values are in registers
