@@ -27,6 +27,15 @@ bool apart(const Span& out, std::initializer_list<Span> others) {
     if (overlaps(out, o)) return false;
   return true;
 }
+// the outputs are apart from each other and from the inputs
+bool outputs_apart(std::initializer_list<Span> out, std::initializer_list<Span> in) {
+  for (const Span* a = out.begin(); a != out.end(); ++a) {
+    if (!apart(*a, in)) return false;
+    for (const Span* b = a + 1; b != out.end(); ++b)
+      if (overlaps(*a, *b)) return false;
+  }
+  return true;
+}
 // out is the same tensor as `in` or apart from it
 bool same_or_apart(const Span& out, std::initializer_list<Span> in) {
   for (const Span& i : in)
@@ -57,6 +66,9 @@ size_t param_bytes(const moga_shape& s, const moga_norm& n) { return sizeof(floa
 size_t head_bytes(const moga_shape& s) {
   const Strides d = qkv_strides(s);
   return elem_size(s.dtype) * (size_t)((long long)(s.B - 1) * d.b + (long long)(s.H - 1) * d.h + (long long)(s.N - 1) * d.n + s.D);
+}
+Span position_span(const moga_shape& s, const moga_rope_plan& rope, const int32_t* pos, int32_t pos_per_batch) {
+  return {pos, sizeof(int32_t) * (size_t)(pos_per_batch ? s.B : 1) * s.N * rope.n_axes};
 }
 // Whether a row of the [B, H, N, D] tensor at a shares bytes with a row of the one at b, both with the shape's
 // strides (whose own rows are apart): tensors may lie in one another's gaps, as Q, K and V do in the output of
@@ -179,14 +191,16 @@ bool rows_apart(const moga_shape& s) {
   return true;
 }
 
-// The sorted tensors are apart from their sources and from each other.
-bool sorted_apart(const moga_shape& s, const void* Q, const void* K, const void* V, const void* Qp, const void* Kp,
-                  const void* Vp) {
-  const size_t t = head_bytes(s), u = elem_size(s.dtype) * (size_t)s.B * s.H * s.N * s.k * s.D;
-  const Span in[3] = {{Q, t}, {K, t}, {V, t}}, out[3] = {{Qp, u}, {Kp, u}, {Vp, u}};
-  for (int i = 0; i < 3; ++i)
-    if (!apart(out[i], {in[0], in[1], in[2], out[(i + 1) % 3], out[(i + 2) % 3]})) return false;
-  return true;
+// The outputs of the rotating gather, its workspace among them, are apart from each other and from its inputs.
+bool permute_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const int32_t* pos, int32_t pos_per_batch,
+                        const int32_t* gid, const void* Q, const void* K, const void* V, const int32_t* perm,
+                        const int32_t* inv, const int32_t* offsets, const void* Qp, const void* Kp, const void* Vp,
+                        const void* ws) {
+  const size_t t = head_bytes(s), a = (size_t)s.B * s.N * s.k, u = elem_size(s.dtype) * a * s.H * s.D;
+  const size_t ints = sizeof(int32_t) * a;
+  return outputs_apart({{perm, ints}, {inv, ints}, {offsets, sizeof(int32_t) * (size_t)s.B * (s.M + 1)}, {Qp, u}, {Kp, u}, {Vp, u},
+                        {ws, ws_layout(s).scratch_end}},
+                       {{gid, ints}, {Q, t}, {K, t}, {V, t}, position_span(s, rope, pos, pos_per_batch)});
 }
 
 }  // namespace moga

@@ -172,7 +172,8 @@ moga_status moga_permute_rope(const moga_shape* s, const moga_rope_plan* rope, c
                               size_t ws_bytes, void* stream) {
   moga_status st;
   if (!check_shape(s, &st) || !check_rope(*s, rope, pos, pos_per_batch, &st)) return st;
-  if (s->N > 0 && (Qp == nullptr || Kp == nullptr || Vp == nullptr || !sorted_apart(*s, Q, K, V, Qp, Kp, Vp)))
+  if (s->N > 0 && (Qp == nullptr || Kp == nullptr || Vp == nullptr ||
+                   !permute_rope_apart(*s, *rope, pos, pos_per_batch, gid, Q, K, V, perm, inv, offsets, Qp, Kp, Vp, ws)))
     return MOGA_ERR_INVALID_ARG;
   const RopeCall call{rope, pos, pos_per_batch};
   return permute_whole(s, gid, Q, K, V, perm, inv, offsets, Qp, Kp, Vp, ws, ws_bytes, stream, &call);

@@ -90,8 +90,10 @@ bool check_ws(void* ws, size_t have, size_t need, moga_status* st);
 bool check_rope(const moga_shape& s, const moga_rope_plan* rope, const int32_t* pos, int32_t pos_per_batch,
                 moga_status* st);
 bool rows_apart(const moga_shape& s);
-bool sorted_apart(const moga_shape& s, const void* Q, const void* K, const void* V, const void* Qp, const void* Kp,
-                  const void* Vp);
+bool permute_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const int32_t* pos, int32_t pos_per_batch,
+                        const int32_t* gid, const void* Q, const void* K, const void* V, const int32_t* perm,
+                        const int32_t* inv, const int32_t* offsets, const void* Qp, const void* Kp, const void* Vp,
+                        const void* ws);
 
 // Stage launchers (each returns MOGA_OK or MOGA_ERR_CUDA; arguments already validated).
 moga_status launch_route(const moga_shape& s, const void* X, const float* Wr, const float* bias,

@@ -275,6 +275,31 @@ def test_forward_and_backward_rope_refusals(mb):
     assert lib.moga_backward_rope(*args, *[_p(A)] * 14, _p(Bp), SZ, Z) == 1
 
 
+def _refuses_overlaps(call, inputs, outputs, size):
+    """call(**addresses) refuses every output over an input or another output: at the same address, and over its last
+    bytes (size: the bytes of each)."""
+    at = {name: 0x10000000 * (i + 1) for i, name in enumerate([*inputs, *outputs])}
+    for i, out in enumerate(outputs):
+        for other in [*inputs, *outputs[:i], *outputs[i + 1:]]:
+            assert call(**{**at, out: at[other]}) == 1, (out, other)
+            assert call(**{**at, out: at[other] + (size[other] - 1) // 16 * 16}) == 1, (out, other, "end")
+
+
+def test_permute_rope_refuses_overlaps(mb):
+    sh, plan = mb.make_shape(_cfg(k=2)), mb.make_rope([32, 32], grid=(2, 5))
+    need = mb.moga_scratch_bytes(sh)
+    names = ("gid", "Q", "K", "V", "perm", "inv", "offsets", "Qp", "Kp", "Vp", "ws")
+
+    def call(pos, per=0, **at):
+        return mb.lib.moga_permute_rope(ctypes.byref(sh), ctypes.byref(plan), _p(pos), ctypes.c_int32(per), *[_p(at[n]) for n in names], ctypes.c_size_t(need), Z)
+
+    ints, rows = 4 * 2 * 10 * 2, 4 * 2 * 2 * 10 * 64
+    size = dict(pos=4 * 10 * 2, gid=ints, Q=rows, K=rows, V=rows, perm=ints, inv=ints, offsets=4 * 2 * 5, Qp=2 * rows, Kp=2 * rows, Vp=2 * rows, ws=need)
+    _refuses_overlaps(call, ("pos",) + names[:4], names[4:], size)
+    at = {n: 0x10000000 * (i + 1) for i, n in enumerate(names)}
+    assert call(pos=at["Qp"] - 80, per=1, **at) == 1              # positions of each batch item: twice as long
+
+
 def test_binding_refuses_tensors_of_the_cpu(mb):
     sh = mb.make_shape(_cfg())
     x = torch.zeros(2, 10, 64)
