@@ -203,6 +203,19 @@ bool permute_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const i
                        {{gid, ints}, {Q, t}, {K, t}, {V, t}, position_span(s, rope, pos, pos_per_batch)});
 }
 
+// The outputs of the forward with rotary positions, its workspace among them, are apart from each other and from its
+// inputs; rows of O may lie between rows of Q, K and V.
+bool forward_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const int32_t* pos, int32_t pos_per_batch,
+                        const void* X, const float* Wr, const float* bias, const void* Q, const void* K, const void* V,
+                        const void* O, const int32_t* gid, const float* gate, const int32_t* perm, const int32_t* offsets,
+                        const void* ws) {
+  const size_t t = head_bytes(s), words = 4 * (size_t)s.B * s.N * s.k;
+  const Span g{gid, words}, a{gate, words}, p{perm, words}, f{offsets, sizeof(int32_t) * (size_t)s.B * (s.M + 1)}, w{ws, ws_layout(s).total};
+  return outputs_apart({{O, t}, g, a, p, f, w}, {{X, token_bytes(s)}, {Wr, sizeof(float) * (size_t)s.C * s.M}, {bias, sizeof(float) * (size_t)s.M},
+                                                position_span(s, rope, pos, pos_per_batch)}) &&
+         outputs_apart({g, a, p, f, w}, {{Q, t}, {K, t}, {V, t}}) && !rows_meet(s, O, Q) && !rows_meet(s, O, K) && !rows_meet(s, O, V);
+}
+
 }  // namespace moga
 
 extern "C" {

@@ -352,7 +352,9 @@ moga_status moga_forward_rope(const moga_shape* s, const moga_rope_plan* rope, c
                               int32_t* perm_out, int32_t* offsets_out, void* ws, size_t ws_bytes, void* stream) {
   moga_status st;
   if (!check_shape(s, &st) || !check_rope(*s, rope, pos, pos_per_batch, &st)) return st;
-  if (!rows_apart(*s)) return MOGA_ERR_INVALID_ARG;
+  if (!rows_apart(*s) || (s->N > 0 && !forward_rope_apart(*s, *rope, pos, pos_per_batch, X, Wr, bias, Q, K, V, O, gid_out, gate_out,
+                                                          perm_out, offsets_out, ws)))
+    return MOGA_ERR_INVALID_ARG;
   const RopeCall call{rope, pos, pos_per_batch};
   return forward_whole(s, X, Wr, bias, Q, K, V, O, gid_out, gate_out, perm_out, offsets_out, ws, ws_bytes, stream,
                        &call);

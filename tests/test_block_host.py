@@ -300,6 +300,25 @@ def test_permute_rope_refuses_overlaps(mb):
     assert call(pos=at["Qp"] - 80, per=1, **at) == 1              # positions of each batch item: twice as long
 
 
+def test_forward_rope_refuses_overlaps(mb):
+    plan = mb.make_rope([32, 32], grid=(2, 5))
+    names = ("X", "Wr", "bias", "Q", "K", "V", "O", "gid", "gate", "perm", "offsets", "ws")
+
+    def call(pos, shape=mb.make_shape(_cfg(k=2)), **at):
+        return mb.lib.moga_forward_rope(ctypes.byref(shape), ctypes.byref(plan), _p(pos), ctypes.c_int32(0), *[_p(at[n]) for n in names], SZ, Z)
+
+    words, rows = 4 * 2 * 10 * 2, 4 * 2 * 2 * 10 * 64
+    size = dict(pos=4 * 10 * 2, X=4 * 2 * 10 * 64, Wr=4 * 64 * 4, bias=4 * 4, Q=rows, K=rows, V=rows, O=rows, gid=words, gate=words, perm=words,
+                offsets=4 * 2 * 5, ws=mb.moga_workspace_bytes(mb.make_shape(_cfg(k=2))))
+    _refuses_overlaps(call, ("pos",) + names[:6], names[6:], size)
+    # the rows of Q, K, V and O alternate in one [B, N, 4, H, D] tensor: they may, up to the row
+    packed = mb.make_shape(_cfg(k=2), strides=(10 * 512, 64, 512))
+    at = {n: 0x10000000 * (i + 1) for i, n in enumerate(("pos",) + names)}
+    at.update(shape=packed, Q=A, K=A + 512, V=A + 1024, pos=0, ws=0)
+    assert call(**{**at, "O": A + 1536}) == 3                     # only the workspace is missing
+    assert call(**{**at, "O": A + 1536 - 16}) == 1 and call(**{**at, "O": A + 1024}) == 1 and call(**{**at, "O": A + 512 + 2048}) == 1
+
+
 def test_binding_refuses_tensors_of_the_cpu(mb):
     sh = mb.make_shape(_cfg())
     x = torch.zeros(2, 10, 64)
