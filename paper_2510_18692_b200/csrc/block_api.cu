@@ -216,6 +216,28 @@ bool forward_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const i
          outputs_apart({g, a, p, f, w}, {{Q, t}, {K, t}, {V, t}}) && !rows_meet(s, O, Q) && !rows_meet(s, O, K) && !rows_meet(s, O, V);
 }
 
+// The same for the backward with rotary positions (ws_need: the bytes of its workspace); rows of dQ, dK, dV and dO may lie
+// between one another.
+bool backward_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const int32_t* pos, int32_t pos_per_batch,
+                         const void* Qp, const void* Kp, const void* Vp, const void* Op, const float* lse,
+                         const float* gate, const int32_t* perm, const int32_t* inv, const int32_t* offsets,
+                         const void* dO, const void* dQ, const void* dK, const void* dV, const float* dgate,
+                         const void* ws, size_t ws_need) {
+  const size_t t = head_bytes(s), a = (size_t)s.B * s.N * s.k, u = elem_size(s.dtype) * a * s.H * s.D;
+  const Span in[10] = {{Qp, u}, {Kp, u}, {Vp, u}, {Op, u}, {lse, sizeof(float) * a * s.H}, {gate, 4 * a}, {perm, 4 * a}, {inv, 4 * a},
+                       {offsets, sizeof(int32_t) * (size_t)s.B * (s.M + 1)}, position_span(s, rope, pos, pos_per_batch)};
+  const Span g{dgate, 4 * a}, w{ws, ws_need}, out[3] = {{dQ, t}, {dK, t}, {dV, t}};
+  if (!apart(g, {{dO, t}, w}) || !apart(w, {{dO, t}})) return false;
+  for (const Span& i : in)
+    if (overlaps(g, i) || overlaps(w, i)) return false;
+  for (int j = 0; j < 3; ++j) {
+    if (!apart(out[j], {g, w}) || rows_meet(s, out[j].p, dO) || rows_meet(s, out[j].p, out[(j + 1) % 3].p)) return false;
+    for (const Span& i : in)
+      if (overlaps(out[j], i)) return false;
+  }
+  return true;
+}
+
 }  // namespace moga
 
 extern "C" {

@@ -563,7 +563,9 @@ moga_status moga_backward_rope(const moga_shape* s, const moga_rope_plan* rope, 
                                void* ws, size_t ws_bytes, void* stream) {
   moga_status st;
   if (!check_shape(s, &st) || !check_rope(*s, rope, pos, pos_per_batch, &st)) return st;
-  if (!rows_apart(*s)) return MOGA_ERR_INVALID_ARG;
+  if (!rows_apart(*s) || (s->N > 0 && !backward_rope_apart(*s, *rope, pos, pos_per_batch, Qp, Kp, Vp, Op, lse, gate, perm, inv, offsets, dO,
+                                                           dQ, dK, dV, dgate, ws, bwd_layout(*s).total)))
+    return MOGA_ERR_INVALID_ARG;
   const RopeCall call{rope, pos, pos_per_batch};
   return backward_whole(s, Qp, Kp, Vp, Op, lse, gate, perm, inv, offsets, dO, dQ, dK, dV, dgate, ws, ws_bytes, stream,
                         &call);

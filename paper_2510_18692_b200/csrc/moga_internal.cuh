@@ -98,6 +98,11 @@ bool forward_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const i
                         const void* X, const float* Wr, const float* bias, const void* Q, const void* K, const void* V,
                         const void* O, const int32_t* gid, const float* gate, const int32_t* perm, const int32_t* offsets,
                         const void* ws);
+bool backward_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const int32_t* pos, int32_t pos_per_batch,
+                         const void* Qp, const void* Kp, const void* Vp, const void* Op, const float* lse,
+                         const float* gate, const int32_t* perm, const int32_t* inv, const int32_t* offsets,
+                         const void* dO, const void* dQ, const void* dK, const void* dV, const float* dgate,
+                         const void* ws, size_t ws_need);
 
 // Stage launchers (each returns MOGA_OK or MOGA_ERR_CUDA; arguments already validated).
 moga_status launch_route(const moga_shape& s, const void* X, const float* Wr, const float* bias,

@@ -319,6 +319,25 @@ def test_forward_rope_refuses_overlaps(mb):
     assert call(**{**at, "O": A + 1536 - 16}) == 1 and call(**{**at, "O": A + 1024}) == 1 and call(**{**at, "O": A + 512 + 2048}) == 1
 
 
+def test_backward_rope_refuses_overlaps(mb):
+    plan, sh = mb.make_rope([32, 32], grid=(2, 5)), mb.make_shape(_cfg(k=2))
+    names = ("Qp", "Kp", "Vp", "Op", "lse", "gate", "perm", "inv", "offsets", "dO", "dQ", "dK", "dV", "dgate", "ws")
+
+    def call(pos, shape=sh, **at):
+        return mb.lib.moga_backward_rope(ctypes.byref(shape), ctypes.byref(plan), _p(pos), ctypes.c_int32(0), *[_p(at[n]) for n in names], SZ, Z)
+
+    words, rows = 4 * 2 * 10 * 2, 4 * 2 * 2 * 10 * 64
+    size = dict(pos=4 * 10 * 2, lse=2 * words, gate=words, perm=words, inv=words, offsets=4 * 2 * 5, dO=rows, dQ=rows, dK=rows, dV=rows,
+                dgate=words, ws=mb.moga_backward_workspace_bytes(sh), **{n: 2 * rows for n in names[:4]})
+    _refuses_overlaps(call, ("pos",) + names[:10], names[10:], size)
+    packed = mb.make_shape(_cfg(k=2), strides=(10 * 512, 64, 512))
+    at = {n: 0x10000000 * (i + 1) for i, n in enumerate(names)}
+    at.update(shape=packed, dQ=A + (9 << 32), dK=A + (9 << 32) + 512, dV=A + (9 << 32) + 1024, pos=0, ws=0)
+    last = A + (9 << 32) + 1536
+    assert call(**{**at, "dO": last}) == 3                        # only the workspace is missing
+    assert call(**{**at, "dO": last - 16}) == 1 and call(**{**at, "dO": at["dV"]}) == 1 and call(**{**at, "dO": at["dK"] + 2048}) == 1
+
+
 def test_binding_refuses_tensors_of_the_cpu(mb):
     sh = mb.make_shape(_cfg())
     x = torch.zeros(2, 10, 64)
