@@ -295,7 +295,7 @@ moga_status moga_rope(const moga_shape* s, const moga_rope_plan* rope, const int
   if (!PTR_OK(Q) || !PTR_OK(Qo) || (K == nullptr) != (Ko == nullptr) || !aligned16(K) || !aligned16(Ko) || !rows_apart(*s))
     return MOGA_ERR_INVALID_ARG;
   const size_t t = head_bytes(*s);
-  const Span p{pos, sizeof(int32_t) * (size_t)(pos_per_batch ? s->B : 1) * s->N * rope->n_axes};
+  const Span p = position_span(*s, *rope, pos, pos_per_batch);
   if ((Qo != Q && rows_meet(*s, Qo, Q)) || (Ko != K && rows_meet(*s, Ko, K)) || rows_meet(*s, Qo, K) || rows_meet(*s, Qo, Ko) ||
       rows_meet(*s, Ko, Q) || overlaps({Qo, t}, p) || overlaps({Ko, t}, p))
     return MOGA_ERR_INVALID_ARG;
@@ -315,7 +315,7 @@ moga_status moga_permute_rope_backward(const moga_shape* s, const moga_rope_plan
   const Span in[3] = {{dQp, u}, {dKp, u}, {dVp, u}}, iv{inv, sizeof(int32_t) * (size_t)s->B * T};
   const Span out[3] = {{dQ, t}, {dK, t}, {dV, t}};
   for (int i = 0; i < 3; ++i)
-    if (!apart(out[i], {in[0], in[1], in[2], iv}) || rows_meet(*s, out[i].p, out[(i + 1) % 3].p)) return MOGA_ERR_INVALID_ARG;
+    if (!apart(out[i], {in[0], in[1], in[2], iv, position_span(*s, *rope, pos, pos_per_batch)}) || rows_meet(*s, out[i].p, out[(i + 1) % 3].p)) return MOGA_ERR_INVALID_ARG;
   return launch_rope_ungather(*s, *rope, pos, pos_per_batch, dQp, dKp, dVp, inv, dQ, dK, dV,
                               static_cast<cudaStream_t>(stream));
 }

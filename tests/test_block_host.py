@@ -338,6 +338,20 @@ def test_backward_rope_refuses_overlaps(mb):
     assert call(**{**at, "dO": last - 16}) == 1 and call(**{**at, "dO": at["dV"]}) == 1 and call(**{**at, "dO": at["dK"] + 2048}) == 1
 
 
+def test_permute_rope_backward_refuses_overlaps(mb):
+    plan, sh = mb.make_rope([32, 32], grid=(2, 5)), mb.make_shape(_cfg(k=2))
+    names = ("dQp", "dKp", "dVp", "inv", "dQ", "dK", "dV")
+
+    def call(pos, per=0, **at):
+        return mb.lib.moga_permute_rope_backward(ctypes.byref(sh), ctypes.byref(plan), _p(pos), ctypes.c_int32(per), *[_p(at[n]) for n in names], Z)
+
+    rows = 4 * 2 * 2 * 10 * 64
+    size = dict(pos=4 * 10 * 2, inv=4 * 2 * 10 * 2, dQ=rows, dK=rows, dV=rows, dQp=2 * rows, dKp=2 * rows, dVp=2 * rows)
+    _refuses_overlaps(call, ("pos",) + names[:4], names[4:], size)
+    at = {n: 0x10000000 * (i + 1) for i, n in enumerate(names)}
+    assert call(pos=at["dV"] - 80, per=1, **at) == 1
+
+
 def test_binding_refuses_tensors_of_the_cpu(mb):
     sh = mb.make_shape(_cfg())
     x = torch.zeros(2, 10, 64)
