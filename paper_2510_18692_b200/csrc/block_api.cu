@@ -60,6 +60,7 @@ bool check_norm(const moga_shape* s, const moga_norm* n, moga_status* st) {
 bool check_dropout(const moga_dropout* d) {
   return d != nullptr && d->p >= 0.0 && d->p < 1.0 && (reinterpret_cast<uintptr_t>(d->step) & 7u) == 0;
 }
+Span step_span(const moga_dropout* d) { return {d != nullptr ? d->step : nullptr, sizeof(uint64_t)}; }
 size_t param_bytes(const moga_shape& s, const moga_norm& n) { return sizeof(float) * (size_t)s.C * (n.per_batch ? s.B : 1); }
 
 // Extent of the [B, H, N, D] tensor of the shape's strides.
@@ -118,9 +119,9 @@ moga_status norm_forward(const moga_shape* s, const moga_norm* n, const moga_dro
       !aligned4(mean) || !aligned4(rstd))
     return MOGA_ERR_INVALID_ARG;
   const size_t t = token_bytes(*s), p = param_bytes(*s, *n), r = sizeof(float) * (size_t)s->B * s->N;
-  const Span x{X, t}, res{R, t}, h{Hs, t}, y{Y, t}, w{W, p}, b{bias, p}, m{mean, r}, v{rstd, r};
+  const Span x{X, t}, res{R, t}, h{Hs, t}, y{Y, t}, w{W, p}, b{bias, p}, m{mean, r}, v{rstd, r}, step = step_span(d);
   if (!same_or_apart(y, {x, res}) || !same_or_apart(h, {x, res}) || !apart(y, {h, w, b, m, v}) || !apart(h, {w, b, m, v}) ||
-      !apart(m, {x, res, w, b, v}) || !apart(v, {x, res, w, b}))
+      !apart(m, {x, res, w, b, v}) || !apart(v, {x, res, w, b}) || !apart(step, {h, y, m, v}))
     return MOGA_ERR_INVALID_ARG;
   return launch_norm(*s, *n, d, X, R, W, bias, Hs, Y, mean, rstd, static_cast<cudaStream_t>(stream));
 }
@@ -143,7 +144,8 @@ moga_status norm_backward(const moga_shape* s, const moga_norm* n, const moga_dr
       scratch{ws, need};
   if (!same_or_apart(dx, {x, dy, dh}) || !same_or_apart(dr, {x, dy, dh}) || !apart(dx, {dr, w, gw, gb, m, v, scratch}) ||
       !apart(dr, {w, gw, gb, m, v, scratch}) || !apart(gw, {x, dy, dh, w, gb, m, v, scratch}) ||
-      !apart(gb, {x, dy, dh, w, m, v, scratch}) || !apart(scratch, {x, dy, dh, w, m, v}))
+      !apart(gb, {x, dy, dh, w, m, v, scratch}) || !apart(scratch, {x, dy, dh, w, m, v}) ||
+      !apart(step_span(d), {dx, dr, gw, gb, scratch}))
     return MOGA_ERR_INVALID_ARG;
   if (!check_ws(ws, ws_bytes, need, &st)) return st;
   return launch_norm_backward(*s, *n, d, X, W, mean, rstd, dY, dH, dX, dR, dW, dbias, static_cast<char*>(ws), cs);
@@ -265,7 +267,8 @@ moga_status moga_dropout_add(const moga_shape* s, const moga_dropout* d, const v
   if (!check_dropout(d)) return MOGA_ERR_INVALID_ARG;
   if (s->N == 0) return MOGA_OK;
   const size_t t = token_bytes(*s);
-  if (!PTR_OK(X) || !PTR_OK(Y) || !aligned16(R) || !same_or_apart({Y, t}, {{X, t}, {R, t}})) return MOGA_ERR_INVALID_ARG;
+  if (!PTR_OK(X) || !PTR_OK(Y) || !aligned16(R) || !same_or_apart({Y, t}, {{X, t}, {R, t}}) || overlaps({Y, t}, step_span(d)))
+    return MOGA_ERR_INVALID_ARG;
   return launch_dropout(*s, *d, X, R, Y, static_cast<cudaStream_t>(stream));
 }
 

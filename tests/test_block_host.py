@@ -352,6 +352,23 @@ def test_permute_rope_backward_refuses_overlaps(mb):
     assert call(pos=at["dV"] - 80, per=1, **at) == 1
 
 
+def test_dropout_step_word_over_an_output(mb):
+    """The device word that is added to the offset may lie in no output: some blocks would read what others have written."""
+    sh, lib, r, n = mb.make_shape(_cfg()), mb.lib, ctypes.byref, mb.make_norm()
+    drop, need = mb.make_dropout(0.1, 1), mb.moga_layernorm_backward_workspace_bytes(sh, n)
+    t, rows = 4 * 2 * 10 * 64, 4 * 2 * 10
+    for last in (0, 1):
+        for out, size in ((Cp, t), (Dp, t), (Ep, rows), (Fp, rows)):
+            drop.step = out + (size - 8) * last
+            assert lib.moga_residual_norm(r(sh), r(n), r(drop), _p(A), _p(Bp), Z, Z, _p(Cp), _p(Dp), _p(Ep), _p(Fp), Z) == 1, (out, last)
+        for out, size in ((Ep, t), (Fp, t), (Gp, 256), (Hp, 256), (Ip, need)):
+            drop.step = out + (size - 8) * last
+            assert lib.moga_residual_norm_backward(r(sh), r(n), r(drop), _p(A), Z, _p(Bp), _p(Bp + 4096), _p(Cp), _p(Dp), _p(Ep), _p(Fp), _p(Gp), _p(Hp), _p(Ip),
+                                                   ctypes.c_size_t(need), Z) == 1, (out, last)
+        drop.step = Bp + (t - 8) * last
+        assert lib.moga_dropout_add(r(sh), r(drop), _p(A), Z, _p(Bp), Z) == 1
+
+
 def test_binding_refuses_tensors_of_the_cpu(mb):
     sh = mb.make_shape(_cfg())
     x = torch.zeros(2, 10, 64)
