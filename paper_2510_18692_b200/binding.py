@@ -320,6 +320,13 @@ def _ws(where, device, ws):
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
+def _drop(where, device, drop):
+    """The descriptor's address (None: no dropout); its step word, which the kernels read, has to be on their device."""
+    step = getattr(drop, "_step", None)
+    if step is not None and step.get_device() != device:
+        raise MogaError(1, where, f"the dropout's step word is on {step.device}, not on device {device}")
+    return None if drop is None else ctypes.byref(drop)
+
 
 def make_norm(eps=1e-5, per_batch=False) -> MogaNorm:
     return MogaNorm(eps, 1 if per_batch else 0)
@@ -363,7 +370,7 @@ def moga_dropout_add(shape, drop, X, R, Y):
     where = "moga_dropout_add"
     dev = _here(where, X)
     x, r, y = _expect(where, dev, _DTYPES[shape.dtype], shape.B * shape.N * shape.C, X, R, Y)
-    _check(lib.moga_dropout_add(ctypes.byref(shape), ctypes.byref(drop), x, r, y, _stream_of(dev)), where)
+    _check(lib.moga_dropout_add(ctypes.byref(shape), _drop(where, dev, drop), x, r, y, _stream_of(dev)), where)
 
 
 def moga_residual_norm(shape, norm, drop, X, R, W, bias, Hs, Y, mean=None, rstd=None):
@@ -373,8 +380,8 @@ def moga_residual_norm(shape, norm, drop, X, R, W, bias, Hs, Y, mean=None, rstd=
     x, res, h, y = _expect(where, dev, _DTYPES[shape.dtype], rows * shape.C, X, R, Hs, Y)
     w, b = _expect_params(where, dev, shape, norm, W, bias)
     m, r = _expect(where, dev, torch.float32, rows, mean, rstd)
-    _check(lib.moga_residual_norm(ctypes.byref(shape), ctypes.byref(norm), None if drop is None else ctypes.byref(drop),
-                                  x, res, w, b, h, y, m, r, _stream_of(dev)), where)
+    _check(lib.moga_residual_norm(ctypes.byref(shape), ctypes.byref(norm), _drop(where, dev, drop), x, res, w, b, h, y, m, r,
+                                  _stream_of(dev)), where)
 
 
 def moga_residual_norm_backward(shape, norm, drop, Hs, W, mean, rstd, dY, dH, dX, dR, dW, dbias, ws):
@@ -383,9 +390,8 @@ def moga_residual_norm_backward(shape, norm, drop, Hs, W, mean, rstd, dY, dH, dX
     h, dy, dh, dx, dr = _expect(where, dev, _DTYPES[shape.dtype], rows * shape.C, Hs, dY, dH, dX, dR)
     w, dw, db = _expect_params(where, dev, shape, norm, W, dW, dbias)
     m, r = _expect(where, dev, torch.float32, rows, mean, rstd)
-    _check(lib.moga_residual_norm_backward(ctypes.byref(shape), ctypes.byref(norm),
-                                           None if drop is None else ctypes.byref(drop), h, w, m, r, dy, dh, dx, dr, dw,
-                                           db, *_ws(where, dev, ws), _stream_of(dev)), where)
+    _check(lib.moga_residual_norm_backward(ctypes.byref(shape), ctypes.byref(norm), _drop(where, dev, drop), h, w, m, r, dy, dh,
+                                           dx, dr, dw, db, *_ws(where, dev, ws), _stream_of(dev)), where)
 
 
 ROPE_LAYOUTS = {"interleaved": 0, "half": 1}

@@ -383,3 +383,43 @@ def test_binding_refuses_tensors_of_the_cpu(mb):
         mb.moga_rope(sh, mb.make_rope([64]), torch.zeros(9, 1, dtype=torch.int32), q, None, q, None)
     with pytest.raises(mb.MogaError):
         mb.make_dropout(0.1, 0, step=torch.zeros(1, dtype=torch.int64))
+
+
+class _OnDevice:
+    """Stands for a contiguous tensor of a CUDA device."""
+    is_cuda = True
+
+    def __init__(self, *shape, dtype=torch.float32, device=0, at=A):
+        self.shape, self.dtype, self.index, self.at = shape, dtype, device, at
+        self.device = torch.device("cuda", device)
+
+    def get_device(self):
+        return self.index
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def stride(self):
+        return ()
+
+    def data_ptr(self):
+        return self.at
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+
+def test_binding_refuses_a_step_word_of_another_device(mb, monkeypatch):
+    monkeypatch.setattr(mb, "_current_device", lambda: 0)
+    sh, norm = mb.make_shape(_cfg()), mb.make_norm()
+    drop = mb.make_dropout(0.1, 0, step=_OnDevice(1, dtype=torch.int64, device=1, at=Ip))
+    x, r, h, y = (_OnDevice(2, 10, 64, at=at) for at in (A, Bp, Cp, Dp))
+    m, v, ws = _OnDevice(2, 10, at=Ep), _OnDevice(2, 10, at=Fp), _OnDevice(1 << 20, dtype=torch.uint8, at=Gp)
+    for call in (lambda: mb.moga_dropout_add(sh, drop, x, r, y), lambda: mb.moga_residual_norm(sh, norm, drop, x, r, None, None, h, y),
+                 lambda: mb.moga_residual_norm_backward(sh, norm, drop, x, None, m, v, r, None, h, y, None, None, ws)):
+        with pytest.raises(mb.MogaError) as e:
+            call()
+        assert e.value.code == 1 and "step word" in str(e.value)
