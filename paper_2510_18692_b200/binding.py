@@ -409,7 +409,13 @@ def make_rope(axis_dims, layout="interleaved", scaling="none", base=10000.0, fac
     if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
         raise MogaError(1, "make_rope", f"layout {layout!r}, scaling {scaling!r}")
     factors = [factor] * n if isinstance(factor, (int, float)) else list(factor)
-    fill = lambda v, x: list(v)[:n] + [x] * (3 - min(len(list(v)), n))
+    start, grid = list(start), list(grid)
+    if len(factors) != n or len(start) not in (n, 3) or len(grid) != 2:
+        raise MogaError(1, "make_rope", f"factor and start: one for each of the {n} axes; grid: height and width")
+    for name, values in (("axis_dims", axis_dims), ("start", start), ("grid", grid)):
+        if not all(-2 ** 31 <= v < 2 ** 31 for v in values):       # the C side would take the low 32 bits
+            raise MogaError(1, "make_rope", f"{name}: {values} does not fit 32 bits")
+    fill = lambda v, x: v[:n] + [x] * (3 - n)
     cfg = MogaRopeConfig(ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], n, (ctypes.c_int32 * 3)(*fill(axis_dims, 0)),
                          grid[0], grid[1], (ctypes.c_int32 * 3)(*fill(start, 0)), amplitude, base,
                          (ctypes.c_double * 3)(*fill(factors, 1.0)), original_length, beta_slow, beta_fast)

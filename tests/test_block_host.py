@@ -127,6 +127,19 @@ def test_rope_plan_refusals(mb):
     assert e.value.code == 2
 
 
+def test_rope_plan_refuses_what_it_would_cut(mb):
+    """Numbers past 32 bits, and lists that are not one number for each axis."""
+    for kw in (dict(axis_dims=[64], start=(2 ** 31,)), dict(axis_dims=[64], start=(-2 ** 31 - 1,)), dict(axis_dims=[64], start=(2 ** 32 + 5,)),
+               dict(axis_dims=[2 ** 32 + 64]), dict(axis_dims=[32, 32], grid=(1, 2 ** 32 + 7)), dict(axis_dims=[32, 32], grid=(7,)),
+               dict(axis_dims=[32, 32], scaling="linear", factor=[4.0]), dict(axis_dims=[32], scaling="linear", factor=[4.0, 2.0]),
+               dict(axis_dims=[16, 16, 16], start=(5, 1)), dict(axis_dims=[64], start=(5, 1))):
+        with pytest.raises(mb.MogaError) as e:
+            mb.make_rope(**kw)
+        assert e.value.code == 1, kw
+    assert list(mb.make_rope([64], start=(-2 ** 31,)).start) == [-2 ** 31, 0, 0]
+    assert list(mb.make_rope([32, 32], start=(2 ** 31 - 1, 3)).start) == [2 ** 31 - 1, 3, 0]
+
+
 # ---------------------------------------------------------------- refusals of the entry points: nothing is launched
 def _p(addr):
     return ctypes.c_void_p(addr)
