@@ -27,12 +27,14 @@ namespace {
 // 70 % of its time, and reaches 5.9 TB/s where first-come blocks reach 6.8), so the runs shrink: a first tier of
 // one long run for each resident block, then tiers of shorter ones, which the block scheduler hands to whichever
 // SM is free.  Which rows a block has depends on its index alone, so sums over a run keep their order.
+// Where a longest run is set, as many tiers of it come first as it takes; they are stored as one.
 constexpr int kMaxTiers = 48;
 struct Tiers {
   int items, blocks;               // of a tier, blocks for each item
-  int count;
-  int size[kMaxTiers];             // rows of a block
-  int start[kMaxTiers + 1];        // rows of an item before the tier's
+  int count;                       // tiers, of which the first `alike` have the rows of size[0]
+  int alike;
+  int size[kMaxTiers];             // rows of a block, from the last of those tiers on
+  int start[kMaxTiers + 1];        // rows of an item before that tier (start[0]: before the first)
 };
 // rows: of an item (below 2^31); resident: blocks that run at once; most, least: rows of a run.
 inline Tiers make_tiers(long long rows, int items, int resident, int most, int least) {
@@ -41,25 +43,32 @@ inline Tiers make_tiers(long long rows, int items, int resident, int most, int l
   t.blocks = resident / items < 1 ? 1 : resident / items;
   if (t.blocks > rows) t.blocks = (int)rows;
   long long done = 0;
+  int stored = 0;
   while (done < rows) {
     const long long left = rows - done, share = (left + t.blocks - 1) / t.blocks;
-    long long size = t.count == 0 ? share * 5 / 8 : share / 2;
+    long long size = stored == 0 ? share * 5 / 8 : share / 2;
     if (size < least || share - size < least / 2) size = share < 2 * least ? share : least;
-    if (size > most && t.count < kMaxTiers - 12) size = most;
-    if (t.count == kMaxTiers - 1) size = share;
-    t.size[t.count] = (int)size;
-    t.start[t.count++] = (int)done;
+    if (stored == kMaxTiers - 1) size = share;
+    else if (size > most) size = most;
+    if (stored == 0) t.size[stored++] = (int)size;
+    else if (stored > 1 || size != most || t.size[0] != most) {
+      t.start[stored] = (int)done;
+      t.size[stored++] = (int)size;
+    }
+    if (stored == 1) t.alike++;
+    t.count++;
     done += size * t.blocks < left ? size * t.blocks : left;
   }
-  t.start[t.count] = (int)rows;
+  t.start[stored] = (int)rows;
   return t;
 }
 // The run of block `block`: its item, first row inside the item, and rows (0 for the last of an uneven tier).
 __device__ __forceinline__ void block_run(const Tiers& t, int block, int& item, int& lo, int& rows) {
-  const int per = t.items * t.blocks, tier = block / per;
+  const int per = t.items * t.blocks, tier = block / per, at = max(tier - t.alike + 1, 0);
   item = block % per / t.blocks;
-  const int size = t.size[tier], end = t.start[tier + 1];
-  lo = (int)min((long long)t.start[tier] + (long long)(block % t.blocks) * size, (long long)end);
+  const int size = t.size[at], end = t.start[at + 1];
+  const long long first = at > 0 ? t.start[at] : (long long)tier * size * t.blocks;
+  lo = (int)min(first + (long long)(block % t.blocks) * size, (long long)end);
   rows = min(size, end - lo);
 }
 

@@ -216,6 +216,18 @@ def test_workspace_grows_with_the_problem(mb):
             assert partials <= 148 * 8 * math.ceil(cfg.B * cfg.N / (148 * 512)) + items
 
 
+def test_partial_sums_of_the_longest_problems(mb):
+    """A thread adds at most 512 rows in fp32, so a partial row stands for at most 512 rows of each of a block's groups: one of
+    them for rows of 5,120 channels, 16 for 1,000, 32 for 8."""
+    n, per = mb.make_norm(), mb.make_norm(per_batch=True)
+    for norm, cfg, groups in ((per, _cfg(B=300, N=126360, C=5120, dtype="bf16"), 1), (n, _cfg(B=1, N=2 ** 31 - 1, C=8, dtype="bf16"), 32),
+                              (per, _cfg(B=160, N=561600, C=1000, dtype="bf16"), 16), (n, _cfg(B=40, N=561600, C=5120), 1)):
+        items, rows = (cfg.B, cfg.N) if norm is per else (1, cfg.B * cfg.N)
+        partials = (mb.moga_layernorm_backward_workspace_bytes(mb.make_shape(cfg), norm) - 256) // (8 * cfg.C)
+        assert partials >= items * math.ceil(rows / (512 * groups)), cfg
+        assert partials <= 2 * items * math.ceil(rows / (512 * groups)) + 148 * 8
+
+
 def test_dropout_refusals(mb):
     sh, lib, r = mb.make_shape(_cfg()), mb.lib, ctypes.byref
 
