@@ -398,9 +398,11 @@ typedef struct {
 
 /*
  * Y = layer norm of X [B, N, C].  W and bias may be NULL (1 and 0).  mean, rstd [B, N] may be NULL;
- * the backward needs them.  Statistics in fp32, mean and variance in two passes over registers.
- * Y may be X.  C * sizeof(element) <= 32,768 and B * N < 2^31 here and below, else
- * MOGA_ERR_UNSUPPORTED.
+ * the backward needs them.  Statistics in fp32 from one read of the row, without cancellation for rows
+ * far from zero: squares are taken around the mean, or around a mean of some of the row's channels
+ * (each thread's in the kernel of many rows, which then merges means and squares), and the rounding of
+ * that mean is corrected, so a constant row gives bias.  Y may be X.  C * sizeof(element) <= 32,768 and
+ * B * N < 2^31 in the calls with a norm, else MOGA_ERR_UNSUPPORTED.
  */
 moga_status moga_layernorm(const moga_shape* s, const moga_norm* n, const void* X, const float* W, const float* bias,
                            void* Y, float* mean, float* rstd, void* stream);
@@ -458,8 +460,9 @@ moga_status moga_residual_norm_backward(const moga_shape* s, const moga_norm* n,
  *             its temperature goes into amplitude, e.g. 0.1 ln f + 1.
  * Positions: pos [N, n_axes] int32, or [B, N, n_axes] with pos_per_batch = 1; NULL: taken from the
  * token index n: n (one axis), (n / grid_w, n % grid_w), or (frame, y, x) of a video of frames of
- * grid_h x grid_w tokens.  Any 32-bit position keeps its angle to
- * 2^-32 turns: angles are 64-bit fixed-point turns.
+ * grid_h x grid_w tokens.  The phase of any 32-bit position is good to 2^-32 turns (64-bit fixed-point
+ * turns, rounded to 32 bits); the sine and cosine take it as an fp32 number of half turns between -1 and 1,
+ * which moves the angle by at most 2^-26 turns, half a step of fp32 near half a turn.
  */
 typedef enum { MOGA_ROPE_INTERLEAVED = 0, MOGA_ROPE_HALF = 1 } moga_rope_layout;
 typedef enum {
@@ -519,7 +522,8 @@ moga_status moga_permute_rope_backward(const moga_shape* s, const moga_rope_plan
 /*
  * moga_forward and moga_backward of a model with rotary positions: the forward rotates Q and K inside
  * its gather; the backward takes the rotated Qp, Kp (moga_permute_rope) and returns the gradients of the
- * unrotated Q and K, turned back in its last pass.  For the other forms of the forward
+ * unrotated Q and K, turned back in its last pass.  Rows of O may lie between rows of Q, K and V, rows of
+ * dQ, dK, dV and dO between one another; outputs and ws are apart from everything else.  For the other forms of the forward
  * (moga_forward_routed, moga_forward_host, moga_visual_forward) rotate Q and K with moga_rope first.
  */
 moga_status moga_forward_rope(const moga_shape* s, const moga_rope_plan* rope, const int32_t* pos,

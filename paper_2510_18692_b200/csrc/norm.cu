@@ -13,10 +13,10 @@
 // What bounds these kernels on a B200 (times below: bf16, under sustained load, at which the board sits at its
 // power limit and the SMs run at 1.6 - 1.8 GHz instead of 1.97): the HBM while a kernel spends fewer than about
 // two instructions on a byte it moves, above that the issue slots at the lowered clock.
-//   forward, 561,600 x 5,120           1.76 ms, 6.55 TB/s (a device copy of as many bytes: 1.75 ms)
-//   backward, 126,360 x 5,120          0.63 - 0.67 ms, 5.8 - 6.1 TB/s
-//   residual forward, 65,520 x 1,536   0.140 ms, 5.8 TB/s;  fp32, 20,000 x 5,120: 0.249 ms, 6.6 TB/s
-//   residual backward, 32,760 x 5,120  0.303 ms, 5.5 TB/s
+//   forward, 561,600 x 5,120           1.76 - 1.78 ms, 6.5 TB/s (a device copy of as many bytes: 1.75 ms)
+//   backward, 126,360 x 5,120          0.63 - 0.67 ms, 5.8 - 6.1 TB/s;  fp32, 20,000 x 5,120: 0.199 ms, 6.2 TB/s
+//   residual forward, 65,520 x 1,536   0.137 - 0.145 ms, 5.6 - 5.9 TB/s;  fp32, 20,000 x 5,120: 0.242 ms, 6.8 TB/s
+//   residual backward, 32,760 x 5,120  0.303 - 0.319 ms, 5.3 - 5.5 TB/s;  fp32, 20,000 x 5,120: 0.336 ms, 6.1 TB/s
 #include "block_common.cuh"
 
 namespace moga {
@@ -1151,10 +1151,14 @@ BwdPlan bwd_plan(const moga_shape& s, bool per_batch) {
   } else {
     p.tpr = p.threads = (int)align_up((nvec + p.vpt - 1) / p.vpt, 32);
   }
-  // blocks: one to an SM where a block has W in shared memory, else about 640 threads; at least four rows for
-  // each group of threads, and no partial sum over more than 512 rows of a thread.  Equal runs: a partial row
-  // costs as much traffic as three rows, more than shorter runs at the end would level (126,360 x 5,120: 0.65 ms
-  // at full clocks with them, 0.61 without).
+  // blocks: one to an SM where a block has W in shared memory, else as many as make up 640 threads (two at least);
+  // at least four rows for each group of threads, and no partial sum over more than 512 rows of a thread.  The
+  // workspace size, which both forms share and which no CUDA call may be made for, fixes these counts, so they do
+  // not follow what fits an SM in every form: of five blocks of 128 threads four do with the residual (1,544 - 2,048
+  // bf16 channels; 50,000 x 2,048: 212 us, 4.8 TB/s), of two of more than 320 threads one does (fp32, 20,000 x 5,120:
+  // 199 us, 6.2 TB/s); the others start as those end.
+  // Equal runs: a partial row costs as much traffic as three rows, more than shorter runs at the end would level
+  // (126,360 x 5,120: 0.65 ms at full clocks with them, 0.61 without).
   const int groups = p.threads / p.tpr;
   const int per_sm = nvec > 64 && nvec <= 128 ? 1 : 640 / p.threads < 2 ? 2 : 640 / p.threads;
   long long resident = 148ll * per_sm, most = (p.rows * items + 4 * groups - 1) / (4 * groups);
@@ -1307,7 +1311,7 @@ constexpr int kDropUnits = 4;     // units of eight elements in flight per threa
 
 // Y = R + keep X scale, eight elements (one generator call) at a time.  HBM-bound: the generator's forty integer
 // operations for eight elements fit under the 32 to 48 bytes they move (126,360 x 5,120 bf16 with the residual:
-// 0.56 - 0.59 ms, 6.6 - 6.9 TB/s).
+// 0.56 - 0.59 ms, 6.6 - 6.9 TB/s; fp32, 20,000 x 5,120: 176 us, 7.0 TB/s, and without the residual 131 us, 6.3 TB/s).
 template <typename XT, bool RES>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const uint4* X, const uint4* R, uint4* Y, uint64_t nvec,
                                                                const __grid_constant__ DropArgs d) {

@@ -3,15 +3,17 @@
 // Pair j of the rotated channels turns by the angle p theta_j, p the position on the pair's axis:
 // (x, y) -> amplitude (x cos - y sin, x sin + y cos).  Angles are kept in turns as 64-bit fixed point:
 // theta / 2 pi as a fraction of 2^64 (made once, on the host), times the integer position, wraps modulo
-// one turn exactly as the angle does, so the phase of any 32-bit position is good to 2^-33 turns with one
-// integer product, without tables in memory and without fp64 on the device.
+// one turn exactly as the angle does, so the phase of any 32-bit position is good to 2^-32 turns with one
+// integer product, without tables in memory and without fp64 on the device.  The sine and cosine take its upper
+// 32 bits as an fp32 number of half turns between -1 and 1: at most 2^-26 turns more, near half a turn.
 //
 // HBM-bound: each thread forms the cosines and sines of its channels of a token once and applies them to
 // all heads of its share, so the trigonometry is a few percent of the time of the row copies (40 heads of 126,360
 // tokens, Q and K: 0.79 - 0.81 ms, 6.4 - 6.5 TB/s; the inverse gather of a top-2 routing of them: 1.78 ms,
 // 6.5 TB/s).  With one head there is nothing to share it with: 600,000 tokens take 0.13 - 0.16 ms, 3.8 - 4.7 TB/s.
 // Half layouts whose halves are not whole 16-byte vectors use narrower ones (88 of 128 channels, 60,000 tokens,
-// 12 heads: 0.14 ms, 5.2 TB/s; 84 channels: 0.19 ms, 3.8 TB/s; odd halves by shuffles: 0.28 ms, 2.6 TB/s).
+// 12 heads: 0.13 - 0.14 ms, 5.2 - 5.8 TB/s; 84 channels: 0.18 - 0.19 ms, 3.8 - 4.1 TB/s; odd halves by shuffles:
+// 0.28 - 0.29 ms, 2.5 - 2.6 TB/s).
 
 #include <math.h>
 
