@@ -71,6 +71,48 @@ size_t head_bytes(const moga_shape& s) {
 Span position_span(const moga_shape& s, const moga_rope_plan& rope, const int32_t* pos, int32_t pos_per_batch) {
   return {pos, sizeof(int32_t) * (size_t)(pos_per_batch ? s.B : 1) * s.N * rope.n_axes};
 }
+// The axes of the shape's strides, the longest stride first.
+void descending_axes(const moga_shape& s, long long (&stride)[3], long long (&size)[3]) {
+  const Strides d = qkv_strides(s);
+  stride[0] = d.b, stride[1] = d.h, stride[2] = d.n;
+  size[0] = s.B, size[1] = s.H, size[2] = s.N;
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (stride[j] > stride[i]) {
+        const long long t = stride[i], u = size[i];
+        stride[i] = stride[j], size[i] = size[j];
+        stride[j] = t, size[j] = u;
+      }
+}
+// Whether the contiguous tensor c shares bytes with a row of the [B, H, N, D] tensor at a (so it may lie in the gaps
+// between rows, or behind the tokens of a padded batch item).  A row starts at a sum of i stride over the axes and meets c
+// if that lies in (lo, hi).  Axis by axis: a multiple of the stride inside (lo, hi) is such a row, all other indexes 0; else
+// only the last multiple at or below lo has rows that can reach it, as the axes inside a stride extend over less than it.
+// Where they extend over more (rows that share bytes, which inputs may have) the whole extent counts.
+bool touches(const moga_shape& s, const void* a, const Span& c) {
+  if (!overlaps({a, head_bytes(s)}, c)) return false;
+  const long long es = (long long)elem_size(s.dtype);
+  long long stride[3], size[3], lo = (long long)(reinterpret_cast<uintptr_t>(c.p) - reinterpret_cast<uintptr_t>(a)) - s.D * es, hi = lo + s.D * es + (long long)c.bytes;
+  descending_axes(s, stride, size);
+  for (int i = 0; i < 3; ++i) {
+    if (size[i] == 1 || stride[i] == 0) continue;
+    long long inner = 0;
+    for (int j = i + 1; j < 3; ++j) inner += (size[j] - 1) * stride[j];
+    if (inner >= stride[i]) return true;
+    const long long step = stride[i] * es, below = lo < 0 ? -1 : lo / step, next = below + 1;   // below: at or below lo
+    if (next < size[i] && next * step < hi) return true;
+    if (below < 0) return false;                  // lo < 0 and no row starts before hi
+    const long long q = below < size[i] ? below : size[i] - 1;
+    lo -= q * step, hi -= q * step;
+  }
+  return lo < 0 && hi > 0;
+}
+bool any_touches(const moga_shape& s, std::initializer_list<const void*> rows, std::initializer_list<Span> whole) {
+  for (const void* a : rows)
+    for (const Span& c : whole)
+      if (touches(s, a, c)) return true;
+  return false;
+}
 // Whether a row of the [B, H, N, D] tensor at a shares bytes with a row of the one at b, both with the shape's
 // strides (whose own rows are apart): tensors may lie in one another's gaps, as Q, K and V do in the output of
 // one projection.  With delta elements between them it asks for i_b, i_h, i_n with |delta - sum i stride| < D; the
@@ -79,15 +121,8 @@ bool rows_meet(const moga_shape& s, const void* a, const void* b) {
   if (a == nullptr || b == nullptr) return false;
   const long long bytes = (long long)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
   const long long es = (long long)elem_size(s.dtype), delta = bytes >= 0 ? bytes / es : -(-bytes / es);
-  const Strides d = qkv_strides(s);
-  long long stride[3] = {d.b, d.h, d.n}, size[3] = {s.B, s.H, s.N};
-  for (int i = 0; i < 3; ++i)                     // descending
-    for (int j = i + 1; j < 3; ++j)
-      if (stride[j] > stride[i]) {
-        const long long t = stride[i], u = size[i];
-        stride[i] = stride[j], size[i] = size[j];
-        stride[j] = t, size[j] = u;
-      }
+  long long stride[3], size[3];
+  descending_axes(s, stride, size);
   for (int pick = 0; pick < 8; ++pick) {
     long long left = delta;
     bool inside = true;
@@ -198,11 +233,11 @@ bool permute_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const i
                         const int32_t* gid, const void* Q, const void* K, const void* V, const int32_t* perm,
                         const int32_t* inv, const int32_t* offsets, const void* Qp, const void* Kp, const void* Vp,
                         const void* ws) {
-  const size_t t = head_bytes(s), a = (size_t)s.B * s.N * s.k, u = elem_size(s.dtype) * a * s.H * s.D;
-  const size_t ints = sizeof(int32_t) * a;
-  return outputs_apart({{perm, ints}, {inv, ints}, {offsets, sizeof(int32_t) * (size_t)s.B * (s.M + 1)}, {Qp, u}, {Kp, u}, {Vp, u},
-                        {ws, ws_layout(s).scratch_end}},
-                       {{gid, ints}, {Q, t}, {K, t}, {V, t}, position_span(s, rope, pos, pos_per_batch)});
+  const size_t a = (size_t)s.B * s.N * s.k, u = elem_size(s.dtype) * a * s.H * s.D, ints = sizeof(int32_t) * a;
+  const Span p{perm, ints}, i{inv, ints}, f{offsets, sizeof(int32_t) * (size_t)s.B * (s.M + 1)}, q{Qp, u}, k{Kp, u}, v{Vp, u},
+      w{ws, ws_layout(s).scratch_end};
+  return outputs_apart({p, i, f, q, k, v, w}, {{gid, ints}, position_span(s, rope, pos, pos_per_batch)}) &&
+         !any_touches(s, {Q, K, V}, {p, i, f, q, k, v, w});
 }
 
 // The outputs of the forward with rotary positions, its workspace among them, are apart from each other and from its
@@ -211,11 +246,12 @@ bool forward_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const i
                         const void* X, const float* Wr, const float* bias, const void* Q, const void* K, const void* V,
                         const void* O, const int32_t* gid, const float* gate, const int32_t* perm, const int32_t* offsets,
                         const void* ws) {
-  const size_t t = head_bytes(s), words = 4 * (size_t)s.B * s.N * s.k;
-  const Span g{gid, words}, a{gate, words}, p{perm, words}, f{offsets, sizeof(int32_t) * (size_t)s.B * (s.M + 1)}, w{ws, ws_layout(s).total};
-  return outputs_apart({{O, t}, g, a, p, f, w}, {{X, token_bytes(s)}, {Wr, sizeof(float) * (size_t)s.C * s.M}, {bias, sizeof(float) * (size_t)s.M},
-                                                position_span(s, rope, pos, pos_per_batch)}) &&
-         outputs_apart({g, a, p, f, w}, {{Q, t}, {K, t}, {V, t}}) && !rows_meet(s, O, Q) && !rows_meet(s, O, K) && !rows_meet(s, O, V);
+  const size_t words = 4 * (size_t)s.B * s.N * s.k;
+  const Span g{gid, words}, a{gate, words}, p{perm, words}, f{offsets, sizeof(int32_t) * (size_t)s.B * (s.M + 1)}, w{ws, ws_layout(s).total},
+      x{X, token_bytes(s)}, wr{Wr, sizeof(float) * (size_t)s.C * s.M}, b{bias, sizeof(float) * (size_t)s.M},
+      at = position_span(s, rope, pos, pos_per_batch);
+  return outputs_apart({g, a, p, f, w}, {x, wr, b, at}) && !any_touches(s, {Q, K, V, O}, {g, a, p, f, w}) &&
+         !any_touches(s, {O}, {x, wr, b, at}) && !rows_meet(s, O, Q) && !rows_meet(s, O, K) && !rows_meet(s, O, V);
 }
 
 // The same for the backward with rotary positions (ws_need: the bytes of its workspace); rows of dQ, dK, dV and dO may lie
@@ -225,18 +261,15 @@ bool backward_rope_apart(const moga_shape& s, const moga_rope_plan& rope, const 
                          const float* gate, const int32_t* perm, const int32_t* inv, const int32_t* offsets,
                          const void* dO, const void* dQ, const void* dK, const void* dV, const float* dgate,
                          const void* ws, size_t ws_need) {
-  const size_t t = head_bytes(s), a = (size_t)s.B * s.N * s.k, u = elem_size(s.dtype) * a * s.H * s.D;
-  const Span in[10] = {{Qp, u}, {Kp, u}, {Vp, u}, {Op, u}, {lse, sizeof(float) * a * s.H}, {gate, 4 * a}, {perm, 4 * a}, {inv, 4 * a},
-                       {offsets, sizeof(int32_t) * (size_t)s.B * (s.M + 1)}, position_span(s, rope, pos, pos_per_batch)};
-  const Span g{dgate, 4 * a}, w{ws, ws_need}, out[3] = {{dQ, t}, {dK, t}, {dV, t}};
-  if (!apart(g, {{dO, t}, w}) || !apart(w, {{dO, t}})) return false;
-  for (const Span& i : in)
-    if (overlaps(g, i) || overlaps(w, i)) return false;
-  for (int j = 0; j < 3; ++j) {
-    if (!apart(out[j], {g, w}) || rows_meet(s, out[j].p, dO) || rows_meet(s, out[j].p, out[(j + 1) % 3].p)) return false;
-    for (const Span& i : in)
-      if (overlaps(out[j], i)) return false;
-  }
+  const size_t a = (size_t)s.B * s.N * s.k, u = elem_size(s.dtype) * a * s.H * s.D;
+  const std::initializer_list<Span> in = {{Qp, u}, {Kp, u}, {Vp, u}, {Op, u}, {lse, sizeof(float) * a * s.H}, {gate, 4 * a}, {perm, 4 * a},
+                                          {inv, 4 * a}, {offsets, sizeof(int32_t) * (size_t)s.B * (s.M + 1)},
+                                          position_span(s, rope, pos, pos_per_batch)};
+  const Span g{dgate, 4 * a}, w{ws, ws_need};
+  const void* out[3] = {dQ, dK, dV};
+  if (!outputs_apart({g, w}, in) || any_touches(s, {dO, dQ, dK, dV}, {g, w}) || any_touches(s, {dQ, dK, dV}, in)) return false;
+  for (int j = 0; j < 3; ++j)
+    if (rows_meet(s, out[j], dO) || rows_meet(s, out[j], out[(j + 1) % 3])) return false;
   return true;
 }
 
@@ -297,10 +330,9 @@ moga_status moga_rope(const moga_shape* s, const moga_rope_plan* rope, const int
   if (s->N == 0) return MOGA_OK;
   if (!PTR_OK(Q) || !PTR_OK(Qo) || (K == nullptr) != (Ko == nullptr) || !aligned16(K) || !aligned16(Ko) || !rows_apart(*s))
     return MOGA_ERR_INVALID_ARG;
-  const size_t t = head_bytes(*s);
   const Span p = position_span(*s, *rope, pos, pos_per_batch);
   if ((Qo != Q && rows_meet(*s, Qo, Q)) || (Ko != K && rows_meet(*s, Ko, K)) || rows_meet(*s, Qo, K) || rows_meet(*s, Qo, Ko) ||
-      rows_meet(*s, Ko, Q) || overlaps({Qo, t}, p) || overlaps({Ko, t}, p))
+      rows_meet(*s, Ko, Q) || any_touches(*s, {Qo, Ko}, {p}))
     return MOGA_ERR_INVALID_ARG;
   return launch_rope(*s, *rope, pos, pos_per_batch, Q, K, Qo, Ko, transpose != 0, static_cast<cudaStream_t>(stream));
 }
@@ -314,11 +346,10 @@ moga_status moga_permute_rope_backward(const moga_shape* s, const moga_rope_plan
   if (!PTR_OK(dQp) || !PTR_OK(dKp) || !PTR_OK(dVp) || !PTR_OK(inv) || !PTR_OK(dQ) || !PTR_OK(dK) || !PTR_OK(dV) ||
       !rows_apart(*s))
     return MOGA_ERR_INVALID_ARG;
-  const size_t T = (size_t)s->N * s->k, t = head_bytes(*s), u = elem_size(s->dtype) * (size_t)s->B * s->H * T * s->D;
-  const Span in[3] = {{dQp, u}, {dKp, u}, {dVp, u}}, iv{inv, sizeof(int32_t) * (size_t)s->B * T};
-  const Span out[3] = {{dQ, t}, {dK, t}, {dV, t}};
-  for (int i = 0; i < 3; ++i)
-    if (!apart(out[i], {in[0], in[1], in[2], iv, position_span(*s, *rope, pos, pos_per_batch)}) || rows_meet(*s, out[i].p, out[(i + 1) % 3].p)) return MOGA_ERR_INVALID_ARG;
+  const size_t T = (size_t)s->N * s->k, u = elem_size(s->dtype) * (size_t)s->B * s->H * T * s->D;
+  if (any_touches(*s, {dQ, dK, dV}, {{dQp, u}, {dKp, u}, {dVp, u}, {inv, sizeof(int32_t) * (size_t)s->B * T}, position_span(*s, *rope, pos, pos_per_batch)}) ||
+      rows_meet(*s, dQ, dK) || rows_meet(*s, dK, dV) || rows_meet(*s, dV, dQ))
+    return MOGA_ERR_INVALID_ARG;
   return launch_rope_ungather(*s, *rope, pos, pos_per_batch, dQp, dKp, dVp, inv, dQ, dK, dV,
                               static_cast<cudaStream_t>(stream));
 }

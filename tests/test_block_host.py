@@ -363,6 +363,55 @@ def test_backward_rope_refuses_overlaps(mb):
     assert call(**{**at, "dO": last - 16}) == 1 and call(**{**at, "dO": at["dV"]}) == 1 and call(**{**at, "dO": at["dK"] + 2048}) == 1
 
 
+def test_overlaps_are_told_row_by_row(mb):
+    """Strided rows and contiguous tensors around and between them, placed at random: refused (1) if and only if any two share
+    a byte; otherwise only the workspace is missing (3)."""
+    rng, lib, r = np.random.default_rng(5), mb.lib, ctypes.byref
+    plan, base, seen = mb.make_rope([64]), 0x100000000, {1: 0, 3: 0}
+    for _ in range(4000):
+        B, H, N, D, k = int(rng.integers(1, 4)), int(rng.integers(1, 4)), int(rng.integers(1, 5)), 64, 1
+        axes, strides, reach = [("b", B), ("h", H), ("n", N)], {}, D
+        for i in rng.permutation(3):                               # strides whose rows are apart, in any order of the axes
+            name, size = axes[i]
+            strides[name] = reach + 4 * int(rng.choice([0, 0, 4, 16, 40, 200]))
+            reach = (size - 1) * strides[name] + reach if size > 1 else reach
+        cfg = _cfg(B=B, H=H, N=N, k=k)
+        sh = mb.make_shape(cfg, strides=(strides["b"], strides["h"], strides["n"]))
+        extent = 4 * reach
+        at = {"O": base}
+        for t in ("Q", "K", "V"):                                  # far away, or near O
+            at[t] = base + (int(rng.integers(-extent // 16, extent // 16 + 1)) * 16 if rng.random() < 0.4 else (1 << 24) * (1 + "QKV".index(t)))
+        size = dict(gid=4 * B * N, gate=4 * B * N, perm=4 * B * N, offsets=4 * B * 5, X=4 * B * N * 64, Wr=4 * 64 * 4, bias=16, pos=4 * N)
+        for i, t in enumerate(size):
+            at[t] = base + (int(rng.integers(-20, extent // 16 + 4)) * 16 if t in ("gid", "offsets", "pos", "bias") and rng.random() < 0.3 else (1 << 25) * (2 + i))
+        names = ("X", "Wr", "bias", "Q", "K", "V", "O", "gid", "gate", "perm", "offsets")
+        got = lib.moga_forward_rope(r(sh), r(plan), _p(at["pos"]), ctypes.c_int32(0), *[_p(at[n]) for n in names], Z, SZ, Z)
+        rows = np.array([4 * (b * strides["b"] + h * strides["h"] + n * strides["n"]) for b in range(B) for h in range(H) for n in range(N)])
+        spans = {t: [(at[t] + int(o), at[t] + int(o) + 4 * D) for o in rows] for t in "QKVO"} | {t: [(at[t], at[t] + size[t])] for t in size}
+        outs = ("O", "gid", "gate", "perm", "offsets")
+        meet = any(x[0] < y[1] and y[0] < x[1] for o in outs for t in spans if t != o for x in spans[o] for y in spans[t])
+        assert got == (1 if meet else 3), (at, strides, B, H, N)
+        seen[got] += 1
+    assert min(seen.values()) > 500
+
+
+def test_tensors_in_the_gaps_of_padded_rows(mb):
+    """Batch items of up to 64 tokens, of which 10 are used: indexes and sorted rows may lie behind an item's tokens."""
+    lib, r, plan = mb.lib, ctypes.byref, mb.make_rope([64])
+    sh = mb.make_shape(_cfg(), strides=(2 * 64 * 64, 64 * 64, 64))                 # [2, 2, 64, 64], N = 10
+    behind = A + 4 * 10 * 64                                                       # of head 0 of item 0
+    names = ("gid", "Q", "K", "V", "perm", "inv", "offsets", "Qp", "Kp", "Vp")
+    at = {n: 0x10000000 * (i + 1) for i, n in enumerate(names)}
+    at["Q"], need = A, mb.moga_scratch_bytes(sh)
+
+    def call(**kw):
+        return lib.moga_permute_rope(r(sh), r(plan), Z, ctypes.c_int32(0), *[_p({**at, "gid": Bp << 8, **kw}[n]) for n in names], Z, ctypes.c_size_t(need), Z)
+
+    assert call(perm=behind, inv=behind + 256, offsets=behind + 512) == 3
+    assert call(perm=behind - 16) == 1 and call(inv=A + 4 * 64 * 64 - 64) == 1
+    assert call(Qp=behind) == 3 and call(Qp=behind + 8192) == 1                    # 10,240 of the 13,824 bytes before head 1
+
+
 def test_permute_rope_backward_refuses_overlaps(mb):
     plan, sh = mb.make_rope([32, 32], grid=(2, 5)), mb.make_shape(_cfg(k=2))
     names = ("dQp", "dKp", "dVp", "inv", "dQ", "dK", "dV")
